@@ -547,7 +547,8 @@ FAAR_API int faar_embedding(faar_ctx* ctx, int rows, int cols, int vocab, const 
  *                                                    FP32; dx may alias dy or add, not x)
  *   dg = sum over rows of dy h, db = sum over rows of dy    ([cols] float, each nullable; written, not added to)
  *   in an order that the device, rows, cols and whether there is an add decide (no atomics).  cols <= 16384.  workspace: faar_layernorm_workspace_size
- *   bytes, 256-byte aligned, needs no set-up; with neither dg nor db it is not used and may be null.
+ *   bytes, 256-byte aligned, needs no set-up; with neither dg nor db it is not used and may be null.  dg and db are 16-byte
+ *   aligned, as g and b are; mean and rstd, a rotary call's positions and an attention call's lse 4-byte (FAAR_ERR_ALIGN).
  * faar_rope_axes: rotary embedding by positions of several axes (time, height, width), half-split pairing as faar_rope.
  *   positions in: [n_axes, rows] ints.  The head_dim / 2 frequencies are dealt to the axes by axes->sections, whose sum is
  *   head_dim / 2: one section after the other, or (interleaved) frequency i to axis a = i mod n_axes while i < n_axes

@@ -281,6 +281,12 @@ int check_rows_cols(int rows, int cols, std::initializer_list<int64_t> lds, std:
     if (q && !aligned16(q)) return FAAR_ERR_ALIGN;
   return FAAR_OK;
 }
+// FP32 or 32-bit integer operands that a kernel reads or writes one by one
+int check_words(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return FAAR_ERR_ALIGN;
+  return FAAR_OK;
+}
 int check_attention(int batch, int seq, int n_heads, int n_kv_heads, int head_dim, int64_t ldq, int64_t ldkv, int64_t ldo) {
   if (batch <= 0 || seq <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads) return FAAR_ERR_SHAPE;
   if (head_dim != 64 && head_dim != 128) return FAAR_ERR_SHAPE;
@@ -992,6 +998,7 @@ int faar_layernorm(faar_ctx* ctx, int rows, int cols, const void* x, int64_t ldx
   if (!ctx || !x || !g || !y) return FAAR_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || !isfinite(eps)) return FAAR_ERR_INVALID_ARG;
   int st = check_rows_cols(rows, cols, {ldx, ldy}, {x, g, b, y});
+  if (!st) st = check_words({mean, rstd});
   if (st) return st;
   FAAR_DEVICE_GUARD(ctx);
   return cuda_fail(ctx, faar_launch_layernorm(ctx, rows, cols, x, ldx, nullptr, 0, nullptr, 0, g, b, eps, y, ldy, mean, rstd));
@@ -1002,6 +1009,7 @@ int faar_add_layernorm(faar_ctx* ctx, int rows, int cols, const void* a, int64_t
   if (!ctx || !a || !r || !sum || !g || !y) return FAAR_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || !isfinite(eps)) return FAAR_ERR_INVALID_ARG;
   int st = check_rows_cols(rows, cols, {lda, ldr, lds, ldy}, {a, r, sum, g, b, y});
+  if (!st) st = check_words({mean, rstd});
   if (st) return st;
   FAAR_DEVICE_GUARD(ctx);
   return cuda_fail(ctx, faar_launch_layernorm(ctx, rows, cols, a, lda, r, ldr, sum, lds, g, b, eps, y, ldy, mean, rstd));
@@ -1019,6 +1027,7 @@ int faar_layernorm_bwd(faar_ctx* ctx, int rows, int cols, const void* dy, int64_
                        float* db, void* workspace, size_t workspace_bytes) {
   if (!ctx || !dy || !x || !g || !mean || !rstd || !dx) return FAAR_ERR_INVALID_ARG;
   int st = check_rows_cols(rows, cols, {lddy, ldx, lddx}, {dy, x, g, dx, add, dg, db});
+  if (!st) st = check_words({mean, rstd});
   if (st) return st;
   if (cols > FAAR_LAYERNORM_COLS) return FAAR_ERR_SHAPE;
   if (add && (ldadd < cols || ldadd % 8)) return ldadd < cols ? FAAR_ERR_SHAPE : FAAR_ERR_ALIGN;
@@ -1048,6 +1057,7 @@ int faar_rope_axes(faar_ctx* ctx, int rows, int n_heads, int head_dim, const voi
   }
   if (sum != head_dim / 2) return FAAR_ERR_INVALID_ARG;
   int st = check_rows_cols(rows, n_heads * head_dim, {ldx, ldy}, {x, y});
+  if (!st) st = check_words({positions});
   if (st) return st;
   FAAR_DEVICE_GUARD(ctx);
   return cuda_fail(ctx, faar_launch_rope_axes(ctx, rows, n_heads, head_dim, x, ldx, positions, axes, theta, inverse, y, ldy));
@@ -1055,15 +1065,13 @@ int faar_rope_axes(faar_ctx* ctx, int rows, int n_heads, int head_dim, const voi
 
 namespace {
 int check_scored(int batch, int seq, int n_heads, int n_kv_heads, int head_dim, int64_t ldq, int64_t ldkv, int64_t ldo,
-                 const faar_attention_scores* s) {
+                 const faar_attention_scores* s, const float* lse) {
   int st = check_attention(batch, seq, n_heads, n_kv_heads, head_dim, ldq, ldkv, ldo);
   if (st) return st;
   // differences of positions, and the CTAs of a launch (up to four a key tile), in 32 bits
   if (seq > 0x40000000 || (long long)batch * n_heads * (((long long)seq + 127) / 128) > 0x7FFFFFFFll / 4) return FAAR_ERR_SHAPE;
   if (!(s->scale >= 0.f) || !isfinite(s->scale) || !(s->softcap >= 0.f) || !isfinite(s->softcap)) return FAAR_ERR_INVALID_ARG;
-  for (const void* p : {(const void*)s->slopes, (const void*)s->key_lo, (const void*)s->key_hi})
-    if (reinterpret_cast<uintptr_t>(p) & 3u) return FAAR_ERR_ALIGN;
-  return FAAR_OK;
+  return check_words({s->slopes, s->key_lo, s->key_hi, lse});
 }
 // Whether two matrices of `rows` rows share memory: lda, ldb row strides and na, nb row lengths in BF16 elements.  Where the strides are
 // equal their columns may lie side by side in the same rows.
@@ -1081,7 +1089,7 @@ int faar_attention_scored_fwd(faar_ctx* ctx, int batch, int seq, int n_heads, in
                               const void* k, const void* v, int64_t ldkv, const faar_attention_scores* scores, void* out, int64_t ldo,
                               float* lse) {
   if (!ctx || !q || !k || !v || !scores || !out || !lse) return FAAR_ERR_INVALID_ARG;
-  int st = check_scored(batch, seq, n_heads, n_kv_heads, head_dim, ldq, ldkv, ldo, scores);
+  int st = check_scored(batch, seq, n_heads, n_kv_heads, head_dim, ldq, ldkv, ldo, scores, lse);
   if (st) return st;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return FAAR_ERR_ALIGN;
   // outputs are written while others' inputs are still read
@@ -1106,7 +1114,7 @@ int faar_attention_scored_bwd(faar_ctx* ctx, int batch, int seq, int n_heads, in
                               const void* dout, int64_t ldo, const float* lse, void* scratch, size_t scratch_bytes, void* dq, void* dk,
                               void* dv) {
   if (!ctx || !q || !k || !v || !scores || !out || !dout || !lse || !dq || !dk || !dv) return FAAR_ERR_INVALID_ARG;
-  int st = check_scored(batch, seq, n_heads, n_kv_heads, head_dim, ldq, ldkv, ldo, scores);
+  int st = check_scored(batch, seq, n_heads, n_kv_heads, head_dim, ldq, ldkv, ldo, scores, lse);
   if (st) return st;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) ||
       !aligned16(dv))
@@ -1131,8 +1139,7 @@ int faar_attention_scored_bwd(faar_ctx* ctx, int batch, int seq, int n_heads, in
 int faar_attention_ranges(faar_ctx* ctx, int batch, int seq, const int* doc, const int* prefix, int* key_lo, int* key_hi) {
   if (!ctx || !key_lo || !key_hi) return FAAR_ERR_INVALID_ARG;
   if (batch <= 0 || seq <= 0 || (long long)batch * seq > 0x7FFF0000ll) return FAAR_ERR_SHAPE;
-  for (const void* p : {(const void*)doc, (const void*)prefix, (const void*)key_lo, (const void*)key_hi})
-    if (reinterpret_cast<uintptr_t>(p) & 3u) return FAAR_ERR_ALIGN;
+  if (check_words({doc, prefix, key_lo, key_hi})) return FAAR_ERR_ALIGN;
   // a chunk of tokens reads its neighbours' ids and flags
   const uintptr_t bytes = (uintptr_t)batch * seq * sizeof(int);
   auto meets = [&](const int* a, const int* b) {

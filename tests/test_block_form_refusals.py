@@ -1,0 +1,43 @@
+"""Pointers that the calls beyond the causal Llama form have to refuse before anything is launched: without a GPU, on a context that no
+call may get as far as using."""
+import ctypes as C
+
+import pytest
+
+from paper_2603_22370_b200 import build as faar_build
+from paper_2603_22370_b200 import faar
+
+AT = 1 << 20                                                   # an address that is aligned to anything; never followed
+ODD = AT + 2
+
+
+@pytest.fixture(scope="module")
+def refused():
+    faar_build.build()
+    lib = faar.lib()
+    blank = C.create_string_buffer(b"\x7f" * 4096, 4096)      # no such device: a call that is not refused fails there
+
+    def status(name, *args):
+        return getattr(lib, name)(C.addressof(blank), *args)
+
+    return status
+
+
+def with_one_odd(args, which):
+    return [ODD if i == which else a for i, a in enumerate(args)]
+
+
+@pytest.mark.parametrize("name,args,words", [
+    ("faar_layernorm", (4, 64, AT, 64, AT, AT, 1e-5, AT, 64, AT, AT), (9, 10)),
+    ("faar_add_layernorm", (4, 64, AT, 64, AT, 64, AT, 64, AT, AT, 1e-5, AT, 64, AT, AT), (13, 14)),
+    ("faar_layernorm_bwd", (4, 64, AT, 64, AT, 64, AT, AT, AT, None, 0, AT, 64, None, None, None, 0), (7, 8)),
+    ("faar_rope_axes", (4, 1, 64, AT, 64, AT, "axes", 1e4, 0, AT, 64), (5,)),
+    ("faar_attention_scored_fwd", (1, 8, 1, 1, 64, AT, 64, 2 * AT, 3 * AT, 64, "scores", 4 * AT, 64, AT), (13,)),
+    ("faar_attention_scored_bwd", (1, 8, 1, 1, 64, AT, 64, 2 * AT, 3 * AT, 64, "scores", 4 * AT, 5 * AT, 64, AT, AT, 1 << 20, 6 * AT, 7 * AT, 8 * AT), (14,)),
+    ("faar_attention_ranges", (1, 8, AT, 2 * AT, 3 * AT, 4 * AT), (2, 3, 4, 5))])
+def test_words_that_are_not_aligned_are_refused(refused, name, args, words):
+    structs = {"axes": faar.make_rope_axes([16, 8, 8]), "scores": faar.make_attention_scores()}
+    args = [C.byref(structs[a]) if isinstance(a, str) else a for a in args]
+    assert refused(name, *args) == faar.ERR_CUDA               # nothing else is wrong: it gets to the device that is not there
+    for i in words:
+        assert refused(name, *with_one_odd(args, i)) == faar.ERR_ALIGN, i
