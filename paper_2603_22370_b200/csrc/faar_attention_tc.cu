@@ -401,15 +401,26 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __noinline__ void scrub(uint32_t base, int units, int first, int threads) {
+__device__ __noinline__ bool scrub(uint32_t base, int units, int first, int threads) {      // whether there was something to set to 0
+  bool any = false;
   for (int u = first; u < units; u += threads) {
     const uint32_t at = base + 16u * (uint32_t)u;
     const uint4 v = lds128(at);
-    if (not_finite(v))
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(only_finite(v.x)), "r"(only_finite(v.y)), "r"(only_finite(v.z)),
-                   "r"(only_finite(v.w)) : "memory");
+    if (!not_finite(v)) continue;
+    any = true;
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(only_finite(v.x)), "r"(only_finite(v.y)), "r"(only_finite(v.z)),
+                 "r"(only_finite(v.w)) : "memory");
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  return any;
+}
+// Whether a row of HD values in memory holds one that is not finite
+template <int HD>
+__device__ __forceinline__ bool row_not_finite(const __nv_bfloat16* row) {
+  bool any = false;
+#pragma unroll 4
+  for (int c = 0; c < HD; c += 8) any |= not_finite(*reinterpret_cast<const uint4*>(row + c));
+  return any;
 }
 // NaN if one of N products is not finite, else 0 (+ acc)
 template <int N>
@@ -1025,6 +1036,7 @@ template <int HD> struct Dq {
 constexpr int BWD_THREADS = 288, ROW_THREADS = 256;
 
 struct TcBwdParams {
+  const __nv_bfloat16* k;          // as the copies' maps have it: looked at again where something was not finite
   const float* lse; const float* dsum;
   __nv_bfloat16* dq; __nv_bfloat16* dk; __nv_bfloat16* dv;
   long long ldq, ldk;
@@ -1083,6 +1095,26 @@ __device__ __forceinline__ void turn_back(const float2* angles, long long tokens
   }
 }
 
+// What was taken out of a staged row of K for those who do not see it, those who do get all the same: a row of dS K with such a key is no
+// number, whatever dS is (0 times an infinity, too).  Tiles that all of a CTA's queries see get there by themselves; where an edge tile's
+// were set to 0, this looks at the keys of the CTA's span once more, in memory: whether one that the thread's query (`range`) sees has one.
+// All row threads call it; `words`: 8 ints of shared memory.
+__device__ __forceinline__ void row_threads_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(ROW_THREADS) : "memory"); }
+template <int HD>
+__device__ __noinline__ bool sees_bad_key(const __nv_bfloat16* k, long long ldk, Span span, int2 range, volatile uint32_t* words) {
+  bool sees = false;
+  for (int k0 = span.lo; k0 < span.hi; k0 += ROW_THREADS) {
+    const int key = k0 + (int)threadIdx.x;
+    const uint32_t bad = __ballot_sync(0xffffffffu, key < span.hi && row_not_finite<HD>(k + key * ldk));
+    row_threads_sync();                                     // the words of the keys before have been read
+    if ((threadIdx.x & 31) == 0) words[threadIdx.x >> 5] = bad;
+    row_threads_sync();
+#pragma unroll 1
+    for (int w = 0; w < ROW_THREADS / 32; ++w) sees |= (words[w] & range_bits(range, k0 + 32 * w)) != 0u;
+  }
+  return sees;
+}
+
 template <int HD, int FORM>
 __global__ void __launch_bounds__(BWD_THREADS, Dq<HD>::CTAS)
 attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDO,
@@ -1102,6 +1134,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   auto kvfull = [&](int s) { return ctl + 8u + 8u * s; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_CTL + 96);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 100);
+  volatile int* scrubbed = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 224);      // over ranges: K had something that is not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // one-dimensional grid, query tile slowest and descending: CTAs start in order of decreasing work
@@ -1120,6 +1153,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     for (int s = 0; s < (C::TWO ? 2 : 1); ++s) { bar_init(bar_s(s), 1); bar_init(bar_done(s), 1); bar_init(bar_ds(s), ROW_THREADS); }
     bar_init(bar_sfree, ROW_THREADS);
     *abort_flag = 0;
+    *scrubbed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -1293,7 +1327,8 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const int st = j % C::STAGES;
             ok = bar_wait(kvfull(st), (uint32_t)((j / C::STAGES) & 1), abort_flag, 0xD15u);
 #pragma unroll
-            for (int c = 0; c < C::NP; ++c) scrub(sK(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, 32 * (warp & 3) + lane, 128);
+            for (int c = 0; c < C::NP; ++c)
+              if (scrub(sK(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, 32 * (warp & 3) + lane, 128)) *scrubbed = 1;
           }
         }
         if constexpr ((FORM & CAPPED) != 0) tanh_values(t, p.sc);
@@ -1371,6 +1406,8 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       __syncthreads();
       if (ok) by = half == 0 ? mine + sums[QT + row] : sums[row] + mine;
       if (ok && half == 0 && qi < p.S) const_cast<float*>(p.dsum)[ro + qi] = (by - nd) / p.inv_sqrt_d;
+      if (*scrubbed && sees_bad_key<HD>(p.k + seq0 * p.ldk + g * HD, p.ldk, span, range, reinterpret_cast<volatile uint32_t*>(sums + 2 * QT)))
+        by = __int_as_float(0x7FFFFFFF);
     }
     if (ok) {
       fence_after();
@@ -2097,6 +2134,7 @@ int faar_launch_attention_scored_bwd(faar_ctx* ctx, int B, int S, int H, int Hkv
   p.lse = lse; p.dsum = delta;
   p.sum_parts = 1; p.sum_head = S; p.sum_batch = (long long)H * S;
   p.dq = reinterpret_cast<__nv_bfloat16*>(dq); p.dk = reinterpret_cast<__nv_bfloat16*>(dk); p.dv = reinterpret_cast<__nv_bfloat16*>(dv);
+  p.k = reinterpret_cast<const __nv_bfloat16*>(k);
   p.ldq = ldq; p.ldk = ldk; p.B = B; p.S = S; p.H = H; p.Hkv = Hkv;
   p.scale_log2 = scale * 1.4426950408889634f; p.inv_sqrt_d = scale;
   p.sc = score_args(scores, scale);
