@@ -383,7 +383,8 @@ __device__ __forceinline__ float2 add_bias(float2 x, float nb, float d) {
 
 // Rows of an operand that some of the rows working with it may not see: what is not finite there would reach them all, as 0 times
 // an infinity is no 0.  Such values of a staged tile are set to 0 (`units` 16-byte units from `base` on, of which the calling thread
-// takes every `threads`-th from `first` on); the generic writes are made visible to the tensor cores.
+// takes every `threads`-th from `first` on; `found`: a flag in shared memory, set where there are any, or 0); the generic writes are made
+// visible to the tensor cores.
 __device__ __forceinline__ bool not_finite(uint4 v) {        // all exponent bits of one of eight BF16 values set
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t acc = 0;
@@ -401,18 +402,21 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __noinline__ bool scrub(uint32_t base, int units, int first, int threads) {      // whether there was something to set to 0
-  bool any = false;
+__device__ __noinline__ void scrub(uint32_t base, int units, int first, int threads, uint32_t found) {
   for (int u = first; u < units; u += threads) {
     const uint32_t at = base + 16u * (uint32_t)u;
     const uint4 v = lds128(at);
     if (!not_finite(v)) continue;
-    any = true;
+    if (found) asm volatile("st.shared.u32 [%0], 1;" ::"r"(found) : "memory");
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(only_finite(v.x)), "r"(only_finite(v.y)), "r"(only_finite(v.z)),
                  "r"(only_finite(v.w)) : "memory");
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  return any;
+}
+__device__ __forceinline__ bool flagged(uint32_t flag) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(flag) : "memory");
+  return v != 0;
 }
 // Whether a row of HD values in memory holds one that is not finite
 template <int HD>
@@ -851,7 +855,7 @@ attn_fwd_scored_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
           const uint32_t low = reinterpret_cast<volatile uint32_t*>(seen)[0], high = reinterpret_cast<volatile uint32_t*>(seen)[1];
           if (low | high) {
             poison |= ((low & range_bits(range, k0)) | (high & range_bits(range, k0 + 32))) != 0u;
-            scrub(sV(st), KV_BYTES / 16, threadIdx.x, 128);
+            scrub(sV(st), KV_BYTES / 16, threadIdx.x, 128, 0u);
           }
         }
         // S_j complete, and with it all products issued before, P V_{j-2} among them: of the two barriers for P V the one of tile j - 1
@@ -1036,7 +1040,8 @@ template <int HD> struct Dq {
 constexpr int BWD_THREADS = 288, ROW_THREADS = 256;
 
 struct TcBwdParams {
-  const __nv_bfloat16* k;          // as the copies' maps have it: looked at again where something was not finite
+  const __nv_bfloat16* k; const __nv_bfloat16* dout;       // as the copies' maps have them: looked at again where something was not finite
+  long long ldo;
   const float* lse; const float* dsum;
   __nv_bfloat16* dq; __nv_bfloat16* dk; __nv_bfloat16* dv;
   long long ldq, ldk;
@@ -1134,7 +1139,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   auto kvfull = [&](int s) { return ctl + 8u + 8u * s; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_CTL + 96);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 100);
-  volatile int* scrubbed = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 224);      // over ranges: K had something that is not finite
+  const uint32_t scrubbed = ctl + 224;                       // over ranges: K had something that is not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // one-dimensional grid, query tile slowest and descending: CTAs start in order of decreasing work
@@ -1153,7 +1158,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     for (int s = 0; s < (C::TWO ? 2 : 1); ++s) { bar_init(bar_s(s), 1); bar_init(bar_done(s), 1); bar_init(bar_ds(s), ROW_THREADS); }
     bar_init(bar_sfree, ROW_THREADS);
     *abort_flag = 0;
-    *scrubbed = 0;
+    asm volatile("st.shared.u32 [%0], 0;" ::"r"(scrubbed) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -1327,8 +1332,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const int st = j % C::STAGES;
             ok = bar_wait(kvfull(st), (uint32_t)((j / C::STAGES) & 1), abort_flag, 0xD15u);
 #pragma unroll
-            for (int c = 0; c < C::NP; ++c)
-              if (scrub(sK(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, 32 * (warp & 3) + lane, 128)) *scrubbed = 1;
+            for (int c = 0; c < C::NP; ++c) scrub(sK(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, 32 * (warp & 3) + lane, 128, scrubbed);
           }
         }
         if constexpr ((FORM & CAPPED) != 0) tanh_values(t, p.sc);
@@ -1406,7 +1410,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       __syncthreads();
       if (ok) by = half == 0 ? mine + sums[QT + row] : sums[row] + mine;
       if (ok && half == 0 && qi < p.S) const_cast<float*>(p.dsum)[ro + qi] = (by - nd) / p.inv_sqrt_d;
-      if (*scrubbed && sees_bad_key<HD>(p.k + seq0 * p.ldk + g * HD, p.ldk, span, range, reinterpret_cast<volatile uint32_t*>(sums + 2 * QT)))
+      if (flagged(scrubbed) && sees_bad_key<HD>(p.k + seq0 * p.ldk + g * HD, p.ldk, span, range, reinterpret_cast<volatile uint32_t*>(sums + 2 * QT)))
         by = __int_as_float(0x7FFFFFFF);
     }
     if (ok) {
@@ -1549,11 +1553,62 @@ __device__ __noinline__ void finish_parts(uint32_t base, uint32_t t_acc, int row
   }
 }
 
+// HD / 2 columns of accumulators of this thread's lane, from `t` on: no numbers where `bad` (the whole warp calls it)
+template <int HD>
+__device__ __forceinline__ void spoil(uint32_t t, bool bad) {
+#pragma unroll 1
+  for (int c = 0; c < HD / 2; c += 16) {
+    float v[16];
+    uint32_t u[16];
+    ld16(t + (uint32_t)c, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = bad ? 0x7FFFFFFFu : __float_as_uint(v[i]);
+    st16(t + (uint32_t)c, u);
+  }
+  wait_st();
+}
+// As sees_bad_key: what was taken out of staged rows of dO for the keys that they do not see makes dV of those that they do no
+// number.  Goes through the queries of all heads of the group once more, in memory, and spoils the accumulators of this CTA's keys
+// that one with such a row sees.  All row threads call it, the products being through.  It finds anew what it works on: with arguments
+// whole and dealt key tiles of heads of 64 kept their registers for them (4 x 2048 tokens, capped, backward call 597 -> 615 us).
+template <int HD, bool DEALT>
+__device__ __noinline__ void spoil_seen(const TcBwdParams& p) {
+  extern __shared__ uint8_t raw[];
+  uint8_t* const smem = raw + (((s32(raw) + 1023u) & ~1023u) - s32(raw));
+  int4* const list = reinterpret_cast<int4*>(smem);         // over the operands, which have been read
+  const uint32_t t_lane = *reinterpret_cast<volatile uint32_t*>(smem + Dkv<HD>::OFF_CTL + 128) + ((threadIdx.x & 96) << 16);
+  const int groups = p.Hkv * p.B, rep = p.H / p.Hkv, tile = (int)(blockIdx.x / (unsigned)(DEALT ? p.parts : 1));
+  const int g = (tile % groups) % p.Hkv, b = (tile % groups) / p.Hkv, row = (int)threadIdx.x & (QT - 1), half = (int)threadIdx.x >> 7;
+  const int kj = tile / groups * QT + row;
+  bool spoilt_v = false;
+  for (int h = g * rep; h < (g + 1) * rep; ++h)
+    for (int q0 = 0; q0 < p.S; q0 += ROW_THREADS) {
+      const int q = q0 + (int)threadIdx.x;
+      int4 mine = make_int4(EMPTY_LO, 0, 0, 0);             // first key, how many, whether dO is not finite
+      if (q < p.S) {
+        const int2 r = key_range(p.sc, b, q, p.S);
+        mine = make_int4(r.x, max(r.y - r.x, 0), row_not_finite<HD>(p.dout + ((long long)b * p.S + q) * p.ldo + h * HD), 0);
+      }
+      row_threads_sync();                                   // the list before has been read
+      list[threadIdx.x] = mine;
+      row_threads_sync();
+#pragma unroll 1
+      for (int i = 0; i < ROW_THREADS; ++i) {
+        const int4 v = list[i];
+        if ((uint32_t)(kj - v.x) < (uint32_t)v.y) spoilt_v |= v.z != 0;
+      }
+    }
+  fence_after();
+  if (__any_sync(0xffffffffu, spoilt_v)) spoil<HD>(t_lane + (uint32_t)(Dkv<HD>::COL_DV + HD / 2 * half), spoilt_v);
+  fence_before();
+  row_threads_sync();                                       // a row's two threads may read one another's columns (finish_parts)
+}
+
 // DEALT: p.parts CTAs share a key tile (compiled in: as a choice at run time it cost whole key tiles 1 %)
 template <int HD, bool DEALT, int FORM>
 __global__ void __launch_bounds__(BWD_THREADS, Dkv<HD>::CTAS)
 attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDO,
-                     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const TcBwdParams p) {
+                     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TcBwdParams p) {
   using C = Dkv<HD>;
   extern __shared__ uint8_t raw[];
   const uint32_t base = (s32(raw) + 1023u) & ~1023u;
@@ -1567,6 +1622,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   auto bar_rv = [&](int s) { return ctl + 112u + 8u * s; };       // 2: lse / delta of an item staged, previous use read by all
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_CTL + 128);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 132);
+  const uint32_t scrubbed_do = ctl + 136;                   // over ranges: dO had something that is not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // one-dimensional grid, key tile slowest: CTAs start in order of decreasing work (the first key tiles see the
@@ -1590,6 +1646,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       bar_init(bar_s(s), 1); bar_init(bar_done(s), 1); bar_init(bar_pds(s), ROW_THREADS); bar_init(bar_rv(s), ROW_THREADS);
     }
     *abort_flag = 0;
+    asm volatile("st.shared.u32 [%0], 0;" ::"r"(scrubbed_do) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -1798,18 +1855,16 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         constexpr bool EDGE = decltype(edge_tag)::value;
         float t[32], d[32];
         ld32x2(t_lane + col_s(i) + 32u * half, t_lane + col_dp(i) + 32u * half, t, d);
-        [[maybe_unused]] bool odd = false;
         if constexpr (FORM != CAUSAL && EDGE) {
           // a row of Q or dO that is not finite shows in its whole column of S^T or dP^T; see the dQ kernel
           const float2 f = finite_probe(d, finite_probe(t, pair(0.f)));
-          odd = __any_sync(0xffffffffu, !(f.x + f.y == 0.f));
-          if (odd) {
+          if (__any_sync(0xffffffffu, !(f.x + f.y == 0.f))) {
             const int st = i % C::STAGES;
             ok = bar_wait(qfull(st), (uint32_t)((i / C::STAGES) & 1), abort_flag, 0xF15u);
 #pragma unroll
             for (int c = 0; c < C::NP; ++c) {
-              scrub(sQ(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128);
-              scrub(sDO(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128);
+              scrub(sQ(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, 0u);
+              scrub(sDO(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed_do);
             }
           }
         }
@@ -1843,13 +1898,6 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             d[j] = r.x; d[j + 1] = r.y;
           }
         }
-        if constexpr (FORM != CAUSAL && EDGE) {
-          if (odd) {                                             // where dO has been rid of what is not finite, dV learns of it from dS
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!(fabsf(d[j]) < INFINITY)) t[j] = __int_as_float(0x7FFFFFFF);
-          }
-        }
         // this thread's half of the rows of P^T and dS^T: A operands in tensor memory
         uint32_t pk[16];
 #pragma unroll
@@ -1872,6 +1920,10 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (ok && n_it > 0) {
       ok = bar_wait(bar_done((n_it - 1) & 1), (uint32_t)(((n_it - 1) >> 1) & 1), abort_flag, 0xF30u);
       ok = __all_sync(0xffffffffu, ok);
+    }
+    if constexpr (FORM != CAUSAL) {
+      row_threads_sync();                                     // all have come to the end: the flag is final, the operands have been read
+      if (flagged(scrubbed_do)) spoil_seen<HD, DEALT>(p);
     }
     if constexpr (DEALT) {
       fence_after();
@@ -2134,7 +2186,7 @@ int faar_launch_attention_scored_bwd(faar_ctx* ctx, int B, int S, int H, int Hkv
   p.lse = lse; p.dsum = delta;
   p.sum_parts = 1; p.sum_head = S; p.sum_batch = (long long)H * S;
   p.dq = reinterpret_cast<__nv_bfloat16*>(dq); p.dk = reinterpret_cast<__nv_bfloat16*>(dk); p.dv = reinterpret_cast<__nv_bfloat16*>(dv);
-  p.k = reinterpret_cast<const __nv_bfloat16*>(k);
+  p.k = reinterpret_cast<const __nv_bfloat16*>(k); p.dout = reinterpret_cast<const __nv_bfloat16*>(dout); p.ldo = ldo;
   p.ldq = ldq; p.ldk = ldk; p.B = B; p.S = S; p.H = H; p.Hkv = Hkv;
   p.scale_log2 = scale * 1.4426950408889634f; p.inv_sqrt_d = scale;
   p.sc = score_args(scores, scale);

@@ -67,3 +67,34 @@ def test_an_infinite_key_leaves_no_gradient_to_those_who_see_it(ctx, D, cap, val
         dq, dq0 = got[2][:, h * D:(h + 1) * D], clean[2][:, h * D:(h + 1) * D]
         assert broken(dq[see]).all()
         assert torch.equal(dq[rest], dq0[rest])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [INF, -INF, float("nan")])
+@pytest.mark.parametrize("at", PLACES)
+def test_values_do_not_enter_the_gradient_of_values(ctx, D, value, at):  # noqa: F811
+    """dV = P^T dO: a v that is no number leaves it as it is, while the outputs, dQ and dK of those who see it are no numbers."""
+    c = Case(1, S, 2, 1, D, *ranges_of_two_documents(S, CUT), 20.0, pad=0)
+    clean, got = runs(ctx, c, "v", at, value)
+    see, rest = who_sees(at)
+    assert torch.equal(got[4], clean[4])
+    assert broken(got[0][see]).all() and broken(got[2][see]).all()
+    assert torch.equal(got[0][rest], clean[0][rest]) and torch.equal(got[2][rest], clean[2][rest])
+
+
+@pytest.mark.parametrize("heads", [(2, 1, 1), (8, 2, 3)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [INF, float("nan")])
+@pytest.mark.parametrize("at", PLACES)
+def test_a_gradient_that_is_no_number_reaches_the_values_that_were_seen(ctx, D, value, at, heads):  # noqa: F811
+    H, G, B = heads
+    lo, hi = (np.repeat(a, B, 0) for a in ranges_of_two_documents(S, CUT))
+    c = Case(B, S, H, G, D, lo, hi, 0.0, pad=0)
+    clean, got = runs(ctx, c, "do", at, value)
+    seen, rest = whom_it_sees(at)
+    rest = rest + list(range(S, B * S))                          # and the other sequences
+    for i in (3, 4):
+        for g in range(G):
+            cols = slice(g * D, (g + 1) * D)
+            assert broken(got[i][seen][:, cols]).all() and torch.equal(got[i][rest][:, cols], clean[i][rest][:, cols])
+    assert torch.equal(got[0], clean[0])
