@@ -617,8 +617,8 @@ FAAR_API int faar_attention_bwd(faar_ctx* ctx, int batch, int seq, int n_heads, 
  * query sees gets dk = dv = 0.  What a token may not see does not reach it, infinities and NaN included: a query's results
  * depend on its own q and on the k and v of its range alone, and gradients likewise.  A query that does see a v with an
  * infinity or NaN has NaN or infinities in its output (not necessarily in the same columns alone), and so has the dq of one that
- * sees such a k, even where its output is finite (0 times an infinity is no number), and a key's gradient from such a q or
- * dout.  Results are reproducible (no atomics).  No gradient is formed towards slopes.  out shares no memory with q,
+ * sees such a k, even where its output is finite (0 times an infinity is no number), and so have a key's dk from such a q and its
+ * dv from such a dout.  Results are reproducible (no atomics).  No gradient is formed towards slopes.  out shares no memory with q,
  * k or v (FAAR_ERR_INVALID_ARG; columns side by side in the same rows are fine). */
 typedef struct {
   float scale;            /* of the scores; 0: 1 / sqrt(head_dim).  Positive and finite                     */

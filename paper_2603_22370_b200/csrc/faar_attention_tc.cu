@@ -1040,7 +1040,7 @@ template <int HD> struct Dq {
 constexpr int BWD_THREADS = 288, ROW_THREADS = 256;
 
 struct TcBwdParams {
-  const __nv_bfloat16* k; const __nv_bfloat16* dout;       // as the copies' maps have them: looked at again where something was not finite
+  const __nv_bfloat16* q; const __nv_bfloat16* k; const __nv_bfloat16* dout;       // as the copies' maps have them: looked at again where something was not finite
   long long ldo;
   const float* lse; const float* dsum;
   __nv_bfloat16* dq; __nv_bfloat16* dk; __nv_bfloat16* dv;
@@ -1567,8 +1567,8 @@ __device__ __forceinline__ void spoil(uint32_t t, bool bad) {
   }
   wait_st();
 }
-// As sees_bad_key: what was taken out of staged rows of dO for the keys that they do not see makes dV of those that they do no
-// number.  Goes through the queries of all heads of the group once more, in memory, and spoils the accumulators of this CTA's keys
+// As sees_bad_key: what was taken out of staged rows of Q or dO for the keys that they do not see makes dK or dV of those that they do
+// no number.  Goes through the queries of all heads of the group once more, in memory, and spoils the accumulators of this CTA's keys
 // that one with such a row sees.  All row threads call it, the products being through.  It finds anew what it works on: with arguments
 // whole and dealt key tiles of heads of 64 kept their registers for them (4 x 2048 tokens, capped, backward call 597 -> 615 us).
 template <int HD, bool DEALT>
@@ -1580,14 +1580,15 @@ __device__ __noinline__ void spoil_seen(const TcBwdParams& p) {
   const int groups = p.Hkv * p.B, rep = p.H / p.Hkv, tile = (int)(blockIdx.x / (unsigned)(DEALT ? p.parts : 1));
   const int g = (tile % groups) % p.Hkv, b = (tile % groups) / p.Hkv, row = (int)threadIdx.x & (QT - 1), half = (int)threadIdx.x >> 7;
   const int kj = tile / groups * QT + row;
-  bool spoilt_v = false;
+  int seen = 0;                                             // by a query whose q (1), whose dO (2) is not finite
   for (int h = g * rep; h < (g + 1) * rep; ++h)
     for (int q0 = 0; q0 < p.S; q0 += ROW_THREADS) {
       const int q = q0 + (int)threadIdx.x;
-      int4 mine = make_int4(EMPTY_LO, 0, 0, 0);             // first key, how many, whether dO is not finite
+      int4 mine = make_int4(EMPTY_LO, 0, 0, 0);             // first key, how many, which of the two is not finite
       if (q < p.S) {
         const int2 r = key_range(p.sc, b, q, p.S);
-        mine = make_int4(r.x, max(r.y - r.x, 0), row_not_finite<HD>(p.dout + ((long long)b * p.S + q) * p.ldo + h * HD), 0);
+        const long long at = (long long)b * p.S + q;
+        mine = make_int4(r.x, max(r.y - r.x, 0), row_not_finite<HD>(p.q + at * p.ldq + h * HD) + 2 * row_not_finite<HD>(p.dout + at * p.ldo + h * HD), 0);
       }
       row_threads_sync();                                   // the list before has been read
       list[threadIdx.x] = mine;
@@ -1595,11 +1596,13 @@ __device__ __noinline__ void spoil_seen(const TcBwdParams& p) {
 #pragma unroll 1
       for (int i = 0; i < ROW_THREADS; ++i) {
         const int4 v = list[i];
-        if ((uint32_t)(kj - v.x) < (uint32_t)v.y) spoilt_v |= v.z != 0;
+        if ((uint32_t)(kj - v.x) < (uint32_t)v.y) seen |= v.z;
       }
     }
   fence_after();
-  if (__any_sync(0xffffffffu, spoilt_v)) spoil<HD>(t_lane + (uint32_t)(Dkv<HD>::COL_DV + HD / 2 * half), spoilt_v);
+  const uint32_t t_half = t_lane + (uint32_t)(HD / 2 * half);
+  if (__any_sync(0xffffffffu, seen & 1)) spoil<HD>(t_half + (uint32_t)Dkv<HD>::COL_DK, seen & 1);
+  if (__any_sync(0xffffffffu, seen & 2)) spoil<HD>(t_half + (uint32_t)Dkv<HD>::COL_DV, seen & 2);
   fence_before();
   row_threads_sync();                                       // a row's two threads may read one another's columns (finish_parts)
 }
@@ -1622,7 +1625,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   auto bar_rv = [&](int s) { return ctl + 112u + 8u * s; };       // 2: lse / delta of an item staged, previous use read by all
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_CTL + 128);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 132);
-  const uint32_t scrubbed_do = ctl + 136;                   // over ranges: dO had something that is not finite
+  const uint32_t scrubbed = ctl + 136;                   // over ranges: Q or dO had something that is not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // one-dimensional grid, key tile slowest: CTAs start in order of decreasing work (the first key tiles see the
@@ -1646,7 +1649,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       bar_init(bar_s(s), 1); bar_init(bar_done(s), 1); bar_init(bar_pds(s), ROW_THREADS); bar_init(bar_rv(s), ROW_THREADS);
     }
     *abort_flag = 0;
-    asm volatile("st.shared.u32 [%0], 0;" ::"r"(scrubbed_do) : "memory");
+    asm volatile("st.shared.u32 [%0], 0;" ::"r"(scrubbed) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -1863,8 +1866,8 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             ok = bar_wait(qfull(st), (uint32_t)((i / C::STAGES) & 1), abort_flag, 0xF15u);
 #pragma unroll
             for (int c = 0; c < C::NP; ++c) {
-              scrub(sQ(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, 0u);
-              scrub(sDO(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed_do);
+              scrub(sQ(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed);
+              scrub(sDO(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed);
             }
           }
         }
@@ -1923,7 +1926,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     if constexpr (FORM != CAUSAL) {
       row_threads_sync();                                     // all have come to the end: the flag is final, the operands have been read
-      if (flagged(scrubbed_do)) spoil_seen<HD, DEALT>(p);
+      if (flagged(scrubbed)) spoil_seen<HD, DEALT>(p);
     }
     if constexpr (DEALT) {
       fence_after();
@@ -2186,7 +2189,7 @@ int faar_launch_attention_scored_bwd(faar_ctx* ctx, int B, int S, int H, int Hkv
   p.lse = lse; p.dsum = delta;
   p.sum_parts = 1; p.sum_head = S; p.sum_batch = (long long)H * S;
   p.dq = reinterpret_cast<__nv_bfloat16*>(dq); p.dk = reinterpret_cast<__nv_bfloat16*>(dk); p.dv = reinterpret_cast<__nv_bfloat16*>(dv);
-  p.k = reinterpret_cast<const __nv_bfloat16*>(k); p.dout = reinterpret_cast<const __nv_bfloat16*>(dout); p.ldo = ldo;
+  p.q = reinterpret_cast<const __nv_bfloat16*>(q); p.k = reinterpret_cast<const __nv_bfloat16*>(k); p.dout = reinterpret_cast<const __nv_bfloat16*>(dout); p.ldo = ldo;
   p.ldq = ldq; p.ldk = ldk; p.B = B; p.S = S; p.H = H; p.Hkv = Hkv;
   p.scale_log2 = scale * 1.4426950408889634f; p.inv_sqrt_d = scale;
   p.sc = score_args(scores, scale);

@@ -82,7 +82,7 @@ def test_values_do_not_enter_the_gradient_of_values(ctx, D, value, at):  # noqa:
     assert torch.equal(got[0][rest], clean[0][rest]) and torch.equal(got[2][rest], clean[2][rest])
 
 
-@pytest.mark.parametrize("heads", [(2, 1, 1), (8, 2, 3)])
+@pytest.mark.parametrize("heads", [(2, 1, 1), (8, 2, 3), (2, 2, 80)])          # dealt over clusters, and whole key tiles
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("value", [INF, float("nan")])
 @pytest.mark.parametrize("at", PLACES)
@@ -98,3 +98,25 @@ def test_a_gradient_that_is_no_number_reaches_the_values_that_were_seen(ctx, D, 
             cols = slice(g * D, (g + 1) * D)
             assert broken(got[i][seen][:, cols]).all() and torch.equal(got[i][rest][:, cols], clean[i][rest][:, cols])
     assert torch.equal(got[0], clean[0])
+
+
+@pytest.mark.parametrize("heads", [(2, 1, 1), (8, 2, 3), (2, 2, 80)])          # dealt over clusters, and whole key tiles
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("value", [INF, -INF])
+@pytest.mark.parametrize("at", PLACES)
+def test_an_infinite_query_leaves_no_gradient_to_the_keys_that_it_sees(ctx, D, cap, value, at, heads):  # noqa: F811
+    """dK = dS^T Q; with a cap its probabilities, and so dV and its own dQ, are finite."""
+    H, G, B = heads
+    lo, hi = (np.repeat(a, B, 0) for a in ranges_of_two_documents(S, CUT))
+    c = Case(B, S, H, G, D, lo, hi, cap, pad=0)
+    clean, got = runs(ctx, c, "q", at, value)
+    seen, rest = whom_it_sees(at)
+    rest = rest + list(range(S, B * S))
+    for g in range(G):
+        cols = slice(g * D, (g + 1) * D)
+        assert broken(got[3][seen][:, cols]).all()
+        for i in (3, 4):
+            assert torch.equal(got[i][rest][:, cols], clean[i][rest][:, cols])
+    if cap:
+        assert torch.isfinite(got[4]).all() and torch.isfinite(got[2]).all() and torch.isfinite(got[0]).all()
