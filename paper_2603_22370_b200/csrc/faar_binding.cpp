@@ -3,7 +3,8 @@
 // What bounds a small layer is the host: a call through ctypes costs 3-5 us of Python for its dozen tensors and
 // structs, as much as the two or three kernel launches behind it.  Here every entry point that enqueues work becomes
 // a vectorcall function whose argument conversion is generated from the entry point's own C declaration:
-//   pointer            None, an int (address), or a CUDA tensor (its data_ptr(); a host tensor is refused)
+//   pointer            None, an int (address), or a CUDA tensor (its data_ptr(); a host tensor is refused, and as a pointer to
+//                      int any tensor but one of int32: ids and positions are int64 where nobody asked for anything else)
 //   faar_shape /
 //   faar_hparams /
 //   faar_model /
@@ -26,8 +27,10 @@ namespace {
 
 PyObject* s_data_ptr = nullptr;
 PyObject* s_is_cuda = nullptr;
+PyObject* s_dtype = nullptr;
+PyObject* torch_int32 = nullptr;
 
-bool to_address(PyObject* o, void** out) {
+bool to_address(PyObject* o, void** out, bool words) {
   if (o == Py_None) { *out = nullptr; return true; }
   if (PyLong_Check(o)) {
     *out = PyLong_AsVoidPtr(o);
@@ -38,6 +41,13 @@ bool to_address(PyObject* o, void** out) {
   const bool on_device = cuda == Py_True;
   Py_DECREF(cuda);
   if (!on_device) { PyErr_SetString(PyExc_AssertionError, "device tensors only"); return false; }
+  if (words) {
+    PyObject* dtype = PyObject_GetAttr(o, s_dtype);
+    if (!dtype) return false;
+    const bool right = dtype == torch_int32;
+    Py_DECREF(dtype);
+    if (!right) { PyErr_SetString(PyExc_AssertionError, "int32 tensors only"); return false; }
+  }
   PyObject* args[1] = {o};
   PyObject* p = PyObject_VectorcallMethod(s_data_ptr, args, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
   if (!p) return false;
@@ -80,7 +90,7 @@ template <class T> struct Arg<T, std::enable_if_t<std::is_pointer_v<T>>> {
       return true;
     } else {
       void* p;
-      if (!to_address(o, &p)) return false;
+      if (!to_address(o, &p, std::is_same_v<E, int>)) return false;
       v = reinterpret_cast<T>(p);
       return true;
     }
@@ -169,6 +179,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_faarbind", "Calls into libfaar.so
 PyMODINIT_FUNC PyInit__faarbind(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_is_cuda = PyUnicode_InternFromString("is_cuda");
-  if (!s_data_ptr || !s_is_cuda) return nullptr;
+  s_dtype = PyUnicode_InternFromString("dtype");
+  PyObject* torch = PyImport_ImportModule("torch");
+  if (!torch) return nullptr;
+  torch_int32 = PyObject_GetAttrString(torch, "int32");      // kept, as the names are
+  Py_DECREF(torch);
+  if (!s_data_ptr || !s_is_cuda || !s_dtype || !torch_int32) return nullptr;
   return PyModule_Create(&module);
 }

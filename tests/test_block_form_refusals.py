@@ -3,6 +3,7 @@ call may get as far as using."""
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2603_22370_b200 import build as faar_build
 from paper_2603_22370_b200 import faar
@@ -41,3 +42,35 @@ def test_words_that_are_not_aligned_are_refused(refused, name, args, words):
     assert refused(name, *args) == faar.ERR_CUDA               # nothing else is wrong: it gets to the device that is not there
     for i in words:
         assert refused(name, *with_one_odd(args, i)) == faar.ERR_ALIGN, i
+
+
+class DeviceTensor:
+    """What the marshalling asks a tensor for."""
+    is_cuda = True
+
+    def __init__(self, dtype):
+        self.dtype = dtype
+
+    def data_ptr(self):
+        return AT
+
+
+INT_CALLS = [("faar_attention_ranges", (1, 8, "int", 2 * AT, 3 * AT, 4 * AT)), ("faar_attention_ranges", (1, 8, 2 * AT, "int", 3 * AT, 4 * AT)),
+             ("faar_attention_ranges", (1, 8, None, None, 3 * AT, "int")), ("faar_rope_axes", (4, 1, 64, AT, 64, "int", "axes", 1e4, 0, AT, 64)),
+             ("faar_rope", (4, 1, 64, AT, 64, "int", 1e4, 0, AT, 64)), ("faar_embedding", (4, 64, 100, AT, 64, "int", AT, 64))]
+
+
+@pytest.mark.parametrize("name,args", INT_CALLS)
+def test_ids_and_positions_of_another_type_are_refused(name, args):
+    """64-bit ones would be read as twice as many of 32 bits."""
+    faar_build.build()
+    blank = C.create_string_buffer(b"\x7f" * 4096, 4096)
+
+    def status(dtype):
+        return getattr(faar._fast(), name)(C.addressof(blank), *({"int": DeviceTensor(dtype), "axes": faar.make_rope_axes([16, 8, 8])}.get(a, a)
+                                                                 if isinstance(a, str) else a for a in args))
+
+    assert status(torch.int32) == faar.ERR_CUDA                # nothing is wrong: it gets to the device that is not there
+    for dtype in (torch.int64, torch.int16, torch.uint8, torch.bool, torch.float32):
+        with pytest.raises(AssertionError):
+            status(dtype)
