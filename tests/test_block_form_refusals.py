@@ -74,3 +74,42 @@ def test_ids_and_positions_of_another_type_are_refused(name, args):
     for dtype in (torch.int64, torch.int16, torch.uint8, torch.bool, torch.float32):
         with pytest.raises(AssertionError):
             status(dtype)
+
+
+MB = 1 << 20
+FWD = dict(batch=1, seq=64, n_heads=2, n_kv_heads=1, head_dim=64, q=1 * MB, ldq=128, k=2 * MB, v=3 * MB, ldkv=64, scores={}, out=4 * MB, ldo=128, lse=5 * MB)
+BWD = dict(batch=1, seq=64, n_heads=2, n_kv_heads=1, head_dim=64, q=1 * MB, ldq=128, k=2 * MB, v=3 * MB, ldkv=64, scores={}, out=4 * MB, dout=6 * MB, ldo=128,
+           lse=5 * MB, scratch=7 * MB, scratch_bytes=64 * 2 * 4 + 16, dq=8 * MB, dk=9 * MB, dv=10 * MB)
+INF, NAN = float("inf"), float("nan")
+SHARED = [(dict(head_dim=32), faar.ERR_SHAPE), (dict(head_dim=256, ldq=512, ldo=512, ldkv=256), faar.ERR_SHAPE), (dict(n_heads=3, n_kv_heads=2, ldq=192, ldo=192, ldkv=128), faar.ERR_SHAPE),
+          (dict(batch=0), faar.ERR_SHAPE), (dict(seq=0), faar.ERR_SHAPE), (dict(n_heads=0), faar.ERR_SHAPE), (dict(n_kv_heads=0), faar.ERR_SHAPE),
+          (dict(batch=1 << 20, seq=1 << 20), faar.ERR_SHAPE), (dict(batch=1 << 29, seq=1), faar.ERR_SHAPE), (dict(seq=(1 << 30) + 1), faar.ERR_SHAPE),
+          (dict(ldq=64), faar.ERR_SHAPE), (dict(ldo=64), faar.ERR_SHAPE), (dict(ldkv=56), faar.ERR_SHAPE), (dict(ldq=132), faar.ERR_ALIGN), (dict(ldo=132), faar.ERR_ALIGN),
+          (dict(ldkv=68), faar.ERR_ALIGN)]
+SHARED += [({p: None}, faar.ERR_INVALID_ARG) for p in ("q", "k", "v", "scores", "out", "lse")]
+SHARED += [({p: FWD[p] + 8}, faar.ERR_ALIGN) for p in ("q", "k", "v", "out")]
+SHARED += [(dict(scores=s), faar.ERR_INVALID_ARG) for s in (dict(scale=-1.0), dict(scale=INF), dict(scale=NAN), dict(softcap=-1.0), dict(softcap=INF), dict(softcap=NAN))]
+SHARED += [(dict(scores={p: AT + 2}), faar.ERR_ALIGN) for p in ("slopes", "key_lo", "key_hi")]
+OVER = [(dict(out=FWD[p] + 64 * shift), faar.ERR_INVALID_ARG) for p in ("q", "k", "v") for shift in (0, 1)]
+BACK = [({p: None}, faar.ERR_INVALID_ARG) for p in ("dout", "dq", "dk", "dv")] + [({p: BWD[p] + 8}, faar.ERR_ALIGN) for p in ("dout", "dq", "dk", "dv")]
+BACK += [(dict(scratch=None), faar.ERR_WORKSPACE), (dict(scratch=7 * MB + 8), faar.ERR_WORKSPACE), (dict(scratch_bytes=64 * 2 * 4 + 15), faar.ERR_WORKSPACE)]
+BACK += [({p: BWD[o]}, faar.ERR_INVALID_ARG) for p in ("dq", "dk", "dv") for o in ("q", "k", "v", "dout")]
+BACK += [(dict(dk=8 * MB), faar.ERR_INVALID_ARG), (dict(dv=8 * MB), faar.ERR_INVALID_ARG), (dict(dv=9 * MB), faar.ERR_INVALID_ARG)]
+
+
+@pytest.mark.parametrize("name,base,changes", [("faar_attention_scored_fwd", FWD, SHARED + OVER), ("faar_attention_scored_bwd", BWD, SHARED + BACK)])
+def test_attention_over_ranges_refuses_one_wrong_argument_at_a_time(refused, name, base, changes):
+    """The call that is changed in one place is a good one: it gets as far as the device."""
+    def status(**change):
+        a = {**base, **change}
+        if a["scores"] is not None:
+            s = faar.AttentionScores(0.0, 0.0, None, None, None)
+            for key, value in a["scores"].items():
+                setattr(s, key, value)
+            a["scores"] = C.byref(s)
+        return refused(name, *a.values())
+
+    assert status() == faar.ERR_CUDA
+    assert status(scores=dict(scale=0.5, softcap=30.0, slopes=AT, key_lo=AT, key_hi=AT)) == faar.ERR_CUDA
+    for change, want in changes:
+        assert status(**change) == want, change
