@@ -75,14 +75,6 @@ __device__ __forceinline__ void merge(float& m, float& s, float m2, float s2) {
   m = M;
 }
 
-__device__ __forceinline__ void unpack8(const uint4& raw, float (&y)[8]) {      // eight BF16 -> FP32
-  const uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[2 * i] = __uint_as_float(r[i] << 16);
-    y[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
-  }
-}
 __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
 // elements n..7 of a group of eight BF16 replaced by -1e30 (BF16 0xF149)
 __device__ __forceinline__ uint4 mask_tail(uint4 v, int n) {
@@ -156,7 +148,7 @@ align_loss_kernel(const AlignParams p) {
     const float m8 = fmaxf(__low2float(x), __high2float(x)) * p.c;          // tau > 0: scaling keeps the order
     if (m8 > m) { s *= faar_ex2(m - m8); m = m8; }                                // 2^-inf = 0 on the first group
     float z[8];
-    unpack8(v, z);
+    faar_unpack8(v, z);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += faar_ex2(fmaf(z[i], p.c, -m));
   };
@@ -258,8 +250,8 @@ align_loss_kernel(const AlignParams p) {
       const bool last_partial = tail && g == ngroups - 1;
       if (last_partial) { va = mask_tail(va, tail); vb = mask_tail(vb, tail); }
       float a[8], b[8], gr[8];
-      unpack8(va, a);
-      unpack8(vb, b);
+      faar_unpack8(va, a);
+      faar_unpack8(vb, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float pf = faar_ex2(fmaf(a[i], p.c, -lse_f)), pq = faar_ex2(fmaf(b[i], p.c, -lse_q));
@@ -283,8 +275,8 @@ align_loss_kernel(const AlignParams p) {
       for (int g = rank * THREADS + threadIdx.x; 8 * g < p.D; g += CL * THREADS) {
         const int nv = min(8, p.D - 8 * g);
         float a[8], b[8], d[8];
-        unpack8(reinterpret_cast<const uint4*>(hf)[g], a);         // rows are padded to 8 columns (ldh >= ceil8(D))
-        unpack8(reinterpret_cast<const uint4*>(hq)[g], b);
+        faar_unpack8(reinterpret_cast<const uint4*>(hf)[g], a);         // rows are padded to 8 columns (ldh >= ceil8(D))
+        faar_unpack8(reinterpret_cast<const uint4*>(hq)[g], b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           d[i] = b[i] - a[i];
@@ -365,8 +357,8 @@ logit_stats_kernel(const __nv_bfloat16* Z, long long ldz, int V, int T, int slot
       float m = -INFINITY, s = 0.f;
       for (int g = 0; g < n / 16; ++g) {
         float lo[8], hi[8], x[16];
-        unpack8(mine[16 * lane + (2 * g ^ unit)], lo);
-        unpack8(mine[16 * lane + ((2 * g + 1) ^ unit)], hi);
+        faar_unpack8(mine[16 * lane + (2 * g ^ unit)], lo);
+        faar_unpack8(mine[16 * lane + ((2 * g + 1) ^ unit)], hi);
 #pragma unroll
         for (int j = 0; j < 8; ++j) { x[j] = lo[j]; x[8 + j] = hi[j]; }
         faar_stats_update(x, c, m, s);

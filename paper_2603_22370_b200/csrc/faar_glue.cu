@@ -10,24 +10,6 @@ namespace {
 
 constexpr int GL_THREADS = 256;
 
-__device__ __forceinline__ void unpack8(const uint4& raw, float (&x)[8]) {
-  const uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(r[i] << 16);
-    x[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  uint32_t o[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    __nv_bfloat162 p2 = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    o[i] = *reinterpret_cast<uint32_t*>(&p2);
-  }
-  return make_uint4(o[0], o[1], o[2], o[3]);
-}
-
 // Work split of the [rows, 8-element groups] kernels: threadIdx.x / blockIdx.x run over the groups of a row,
 // threadIdx.y / blockIdx.y over rows (grid-stride), so no thread divides its index by the row length.
 struct Split { dim3 grid, block; };
@@ -54,15 +36,15 @@ silu_mul_kernel(const __nv_bfloat16* gate, int64_t ldg, const __nv_bfloat16* up,
       ub = *reinterpret_cast<const uint4*>(up + (int64_t)row1 * ldu + col);
     }
     float a[8], b[8], y[8];
-    unpack8(ga, a); unpack8(ua, b);
+    faar_unpack8(ga, a); faar_unpack8(ua, b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = faar_silu_mul(a[i], b[i]);
-    *reinterpret_cast<uint4*>(out + (int64_t)row * ldo + col) = pack8(y);
+    *reinterpret_cast<uint4*>(out + (int64_t)row * ldo + col) = faar_pack8(y);
     if (two) {
-      unpack8(gb, a); unpack8(ub, b);
+      faar_unpack8(gb, a); faar_unpack8(ub, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = faar_silu_mul(a[i], b[i]);
-      *reinterpret_cast<uint4*>(out + (int64_t)row1 * ldo + col) = pack8(y);
+      *reinterpret_cast<uint4*>(out + (int64_t)row1 * ldo + col) = faar_pack8(y);
     }
   }
 }
@@ -122,11 +104,11 @@ rmsnorm_kernel(const __nv_bfloat16* x, int64_t ldx, const __nv_bfloat16* b, int6
           const int c = lane + 32 * k;
           if (c < n_groups) {
             float a[8], r[8];
-            unpack8(v[k], a);
-            unpack8(*reinterpret_cast<const uint4*>(br + 8 * c), r);
+            faar_unpack8(v[k], a);
+            faar_unpack8(*reinterpret_cast<const uint4*>(br + 8 * c), r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) a[i] += r[i];
-            v[k] = pack8(a);
+            v[k] = faar_pack8(a);
             *reinterpret_cast<uint4*>(sr + 8 * c) = v[k];
           }
         }
@@ -135,7 +117,7 @@ rmsnorm_kernel(const __nv_bfloat16* x, int64_t ldx, const __nv_bfloat16* b, int6
       for (int k = 0; k < NV; ++k) {
         if (lane + 32 * k < n_groups) {
           float a[8];
-          unpack8(v[k], a);
+          faar_unpack8(v[k], a);
 #pragma unroll
           for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], ss);
         }
@@ -148,12 +130,12 @@ rmsnorm_kernel(const __nv_bfloat16* x, int64_t ldx, const __nv_bfloat16* b, int6
         const int c = lane + 32 * k;
         if (c < n_groups) {
           float a[8], o[8];
-          unpack8(v[k], a);
+          faar_unpack8(v[k], a);
           const float4 g0 = *reinterpret_cast<const float4*>(g + 8 * c), g1 = *reinterpret_cast<const float4*>(g + 8 * c + 4);
           const float gg[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = a[i] * rstd * gg[i];
-          *reinterpret_cast<uint4*>(yr + 8 * c) = pack8(o);
+          *reinterpret_cast<uint4*>(yr + 8 * c) = faar_pack8(o);
         }
       }
     } else {
@@ -164,15 +146,15 @@ rmsnorm_kernel(const __nv_bfloat16* x, int64_t ldx, const __nv_bfloat16* b, int6
           if (!known) raw = make_uint4(0u, 0u, 0u, 0u);
           *reinterpret_cast<uint4*>(sr + 8 * c) = raw;
         }
-        unpack8(raw, a);
+        faar_unpack8(raw, a);
         if (br) {
           float r[8];
-          unpack8(*reinterpret_cast<const uint4*>(br + 8 * c), r);
+          faar_unpack8(*reinterpret_cast<const uint4*>(br + 8 * c), r);
 #pragma unroll
           for (int i = 0; i < 8; ++i) a[i] += r[i];
-          const uint4 sum = pack8(a);
+          const uint4 sum = faar_pack8(a);
           *reinterpret_cast<uint4*>(sr + 8 * c) = sum;
-          unpack8(sum, a);
+          faar_unpack8(sum, a);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], ss);
@@ -183,12 +165,12 @@ rmsnorm_kernel(const __nv_bfloat16* x, int64_t ldx, const __nv_bfloat16* b, int6
       const __nv_bfloat16* src = sr ? sr : xr;          // this lane wrote the groups it reads back
       for (int c = lane; c < n_groups; c += 32) {
         float a[8], o[8];
-        unpack8(*reinterpret_cast<const uint4*>(src + 8 * c), a);
+        faar_unpack8(*reinterpret_cast<const uint4*>(src + 8 * c), a);
         const float4 g0 = *reinterpret_cast<const float4*>(g + 8 * c), g1 = *reinterpret_cast<const float4*>(g + 8 * c + 4);
         const float gg[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = a[i] * rstd * gg[i];
-        *reinterpret_cast<uint4*>(yr + 8 * c) = pack8(o);
+        *reinterpret_cast<uint4*>(yr + 8 * c) = faar_pack8(o);
       }
     }
   }
@@ -234,16 +216,16 @@ rmsnorm_bwd_kernel(const __nv_bfloat16* dy, const __nv_bfloat16* dy2, const __nv
     };
     // w = g * (dy + dy2 + dy3) of the k-th requested group
     auto weigh = [&](int k, int c, float (&w)[8]) {
-      unpack8(v1[k], w);
+      faar_unpack8(v1[k], w);
       if (d2) {
         float t[8];
-        unpack8(v2[k], t);
+        faar_unpack8(v2[k], t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] += t[i];
       }
       if (d3) {
         float t[8];
-        unpack8(v3[k], t);
+        faar_unpack8(v3[k], t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] += t[i];
       }
@@ -260,7 +242,7 @@ rmsnorm_bwd_kernel(const __nv_bfloat16* dy, const __nv_bfloat16* dy2, const __nv
         const int c = c0 + 32 * k;
         if (c < n_groups) {
           float a[8], w[8];
-          unpack8(xv[k], a);
+          faar_unpack8(xv[k], a);
           weigh(k, c, w);
 #pragma unroll
           for (int i = 0; i < 8; ++i) dot = fmaf(w[i], a[i] * rstd, dot);
@@ -279,17 +261,17 @@ rmsnorm_bwd_kernel(const __nv_bfloat16* dy, const __nv_bfloat16* dy2, const __nv
         const int c = c0 + 32 * k;
         if (c < n_groups) {
           float a[8], w[8], o[8];
-          unpack8(xv[k], a);
+          faar_unpack8(xv[k], a);
           weigh(k, c, w);
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = rstd * fmaf(-(a[i] * rstd), dot, w[i]);
           if (ar) {
             float r[8];
-            unpack8(av[k], r);
+            faar_unpack8(av[k], r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] += r[i];
           }
-          out[c] = pack8(o);
+          out[c] = faar_pack8(o);
         }
       }
     }
@@ -334,8 +316,8 @@ rmsnorm_bwd_row_kernel(const __nv_bfloat16* dy, int64_t lddy, const __nv_bfloat1
     for (int k = 0; k < NV; ++k) {
       if (lane + 32 * k < n_groups) {
         float a[8], w[8];
-        unpack8(xv[k], a);
-        unpack8(dv[k], w);
+        faar_unpack8(xv[k], a);
+        faar_unpack8(dv[k], w);
         weigh(lane + 32 * k, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dot = fmaf(w[i], a[i] * rstd, dot);
@@ -347,18 +329,18 @@ rmsnorm_bwd_row_kernel(const __nv_bfloat16* dy, int64_t lddy, const __nv_bfloat1
       const int c = lane + 32 * k;
       if (c < n_groups) {
         float a[8], w[8], o[8];
-        unpack8(xv[k], a);
-        unpack8(dv[k], w);
+        faar_unpack8(xv[k], a);
+        faar_unpack8(dv[k], w);
         weigh(c, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = rstd * fmaf(-(a[i] * rstd), dot, w[i]);
         if (ar) {
           float r[8];
-          unpack8(av[k], r);
+          faar_unpack8(av[k], r);
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] += r[i];
         }
-        out[c] = pack8(o);
+        out[c] = faar_pack8(o);
       }
     }
   }
@@ -401,12 +383,12 @@ rope_kernel(const __nv_bfloat16* x, int64_t ldx, const int* __restrict__ pos, __
 #pragma unroll
     for (int h = 0; h < HPT; ++h) {
       float a[8], b[8];
-      unpack8(ra[h], a);
-      unpack8(rb[h], b);
+      faar_unpack8(ra[h], a);
+      faar_unpack8(rb[h], b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) faar_rope_turn(a[i], b[i], sn[i], cs[i]);
-      *reinterpret_cast<uint4*>(yr + h * head_dim) = pack8(a);
-      *reinterpret_cast<uint4*>(yr + h * head_dim + half) = pack8(b);
+      *reinterpret_cast<uint4*>(yr + h * head_dim) = faar_pack8(a);
+      *reinterpret_cast<uint4*>(yr + h * head_dim + half) = faar_pack8(b);
     }
   }
 }
@@ -421,13 +403,13 @@ silu_mul_bwd_kernel(const __nv_bfloat16* dout, int64_t ldd, const __nv_bfloat16*
   const int col = 8 * cg;
   for (int row = split_row0(); row < rows; row += split_row_step()) {
     float d[8], g[8], u[8], og[8], ou[8];
-    unpack8(*reinterpret_cast<const uint4*>(dout + (int64_t)row * ldd + col), d);
-    unpack8(*reinterpret_cast<const uint4*>(gate + (int64_t)row * ldg + col), g);
-    unpack8(*reinterpret_cast<const uint4*>(up + (int64_t)row * ldu + col), u);
+    faar_unpack8(*reinterpret_cast<const uint4*>(dout + (int64_t)row * ldd + col), d);
+    faar_unpack8(*reinterpret_cast<const uint4*>(gate + (int64_t)row * ldg + col), g);
+    faar_unpack8(*reinterpret_cast<const uint4*>(up + (int64_t)row * ldu + col), u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) faar_silu_mul_bwd(d[i], g[i], u[i], og[i], ou[i]);
-    *reinterpret_cast<uint4*>(dgate + (int64_t)row * lddg + col) = pack8(og);
-    *reinterpret_cast<uint4*>(dup + (int64_t)row * lddu + col) = pack8(ou);
+    *reinterpret_cast<uint4*>(dgate + (int64_t)row * lddg + col) = faar_pack8(og);
+    *reinterpret_cast<uint4*>(dup + (int64_t)row * lddu + col) = faar_pack8(ou);
   }
 }
 
@@ -457,11 +439,11 @@ add_kernel(const __nv_bfloat16* a, int64_t lda, const __nv_bfloat16* b, int64_t 
   const int col = 8 * cg;
   for (int row = split_row0(); row < rows; row += split_row_step()) {
     float x[8], y[8], o[8];
-    unpack8(*reinterpret_cast<const uint4*>(a + (int64_t)row * lda + col), x);
-    unpack8(*reinterpret_cast<const uint4*>(b + (int64_t)row * ldb + col), y);
+    faar_unpack8(*reinterpret_cast<const uint4*>(a + (int64_t)row * lda + col), x);
+    faar_unpack8(*reinterpret_cast<const uint4*>(b + (int64_t)row * ldb + col), y);
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = x[i] + y[i];
-    *reinterpret_cast<uint4*>(out + (int64_t)row * ldo + col) = pack8(o);
+    *reinterpret_cast<uint4*>(out + (int64_t)row * ldo + col) = faar_pack8(o);
   }
 }
 
