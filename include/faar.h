@@ -621,8 +621,8 @@ FAAR_API int faar_attention_bwd(faar_ctx* ctx, int batch, int seq, int n_heads, 
  * dv from such a dout.  Results are reproducible (no atomics).  No gradient is formed towards slopes.  out shares no memory with q,
  * k or v (FAAR_ERR_INVALID_ARG; columns side by side in the same rows are fine). */
 typedef struct {
-  float scale;            /* of the scores; 0: 1 / sqrt(head_dim).  Positive and finite                     */
-  float softcap;          /* 0: none.  Positive and finite                                                  */
+  float scale;            /* of the scores; 0: 1 / sqrt(head_dim).  Positive; scale log2(e) a normal float  */
+  float softcap;          /* 0: none.  Positive; softcap log2(e) and scale / softcap normal floats          */
   const float* slopes;    /* [n_heads] device, nullable: none.  Finite                                      */
   const int* key_lo;      /* [batch, seq] device, nullable: 0                                               */
   const int* key_hi;      /* [batch, seq] device, nullable: the query's own position + 1 (causal)           */

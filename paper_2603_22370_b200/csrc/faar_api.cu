@@ -1071,6 +1071,10 @@ int check_scored(int batch, int seq, int n_heads, int n_kv_heads, int head_dim, 
   // differences of positions, and the CTAs of a launch (up to four a key tile), in 32 bits
   if (seq > 0x40000000 || (long long)batch * n_heads * (((long long)seq + 127) / 128) > 0x7FFFFFFFll / 4) return FAAR_ERR_SHAPE;
   if (!(s->scale >= 0.f) || !isfinite(s->scale) || !(s->softcap >= 0.f) || !isfinite(s->softcap)) return FAAR_ERR_INVALID_ARG;
+  // the factors that the kernels multiply by: one that overflows makes a score of 0 no number
+  const double log2e = 1.4426950408889634, scale = s->scale > 0.f ? s->scale : 1.0 / sqrt((double)head_dim);
+  if (!isnormal((float)(scale * log2e))) return FAAR_ERR_INVALID_ARG;
+  if (s->softcap > 0.f && (!isnormal((float)(s->softcap * log2e)) || !isnormal((float)(scale / s->softcap)))) return FAAR_ERR_INVALID_ARG;
   return check_words({s->slopes, s->key_lo, s->key_hi, lse});
 }
 // Whether two matrices of `rows` rows share memory: lda, ldb row strides and na, nb row lengths in BF16 elements.  Where the strides are

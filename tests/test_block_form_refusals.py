@@ -113,3 +113,22 @@ def test_attention_over_ranges_refuses_one_wrong_argument_at_a_time(refused, nam
     assert status(scores=dict(scale=0.5, softcap=30.0, slopes=AT, key_lo=AT, key_hi=AT)) == faar.ERR_CUDA
     for change, want in changes:
         assert status(**change) == want, change
+
+
+@pytest.mark.parametrize("name,base", [("faar_attention_scored_fwd", FWD), ("faar_attention_scored_bwd", BWD)])
+def test_scales_and_caps_whose_factors_are_no_normal_floats_are_refused(refused, name, base):
+    """scale log2(e), softcap log2(e) and scale / softcap are what the kernels multiply scores by: infinite, a score of 0 would be no number,
+    and below the normal range they have no digits left."""
+    least, most = 2.0 ** -126, (2 - 2.0 ** -23) * 2.0 ** 127
+    LOG2E = 1.4426950408889634
+
+    def status(scale, softcap):
+        s = faar.AttentionScores(scale, softcap, None, None, None)
+        return refused(name, *{**base, "scores": C.byref(s)}.values())
+
+    for scale, softcap in [(most, 0.0), (0.7 * most, 0.0), (least / 2, 0.0), (0.0, most), (0.0, 0.7 * most), (0.0, least / 2), (0.0, 2.0 ** 123 * 1.01),
+                           (2.0 ** 64, 2.0 ** -64), (2.0 ** -64, 2.0 ** 63), (0.0, 2.0 ** -131)]:
+        assert status(scale, softcap) == faar.ERR_INVALID_ARG, (scale, softcap)
+    for scale, softcap in [(0.69 * most, 0.0), (least, 0.0), (0.0, 2.0 ** 123), (2.0 ** 63, 2.0 ** -64), (2.0 ** -64, 2.0 ** 62), (0.0, 2.0 ** -126), (0.0, 50.0)]:
+        assert status(scale, softcap) == faar.ERR_CUDA, (scale, softcap)
+    assert 0.69 * LOG2E < 1 < 0.7 * LOG2E
