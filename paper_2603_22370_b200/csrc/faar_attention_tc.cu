@@ -1,7 +1,9 @@
-// Causal attention for head_dim 64 and 128 on the tcgen05 tensor cores (sm_100a): the forward kernel first, then the two
-// backward kernels (dQ; dK and dV), which are built the same way and described where they start.
+// Attention for head_dim 64 and 128 on the tcgen05 tensor cores (sm_100a).  Forward: attn_fwd_tc_kernel for whole causal sequences,
+// attn_fwd_scored_kernel for key ranges with capped or biased scores, a kernel of its own.  Backward: attn_dq_tc_kernel and
+// attn_dkv_tc_kernel are compiled for either (FORM), attn_scored_rows_kernel prepares the forms over ranges.  They are built like the
+// causal forward kernel and described where they start.
 //
-// Forward.  One CTA takes 128 queries of one head and sweeps the keys in tiles of 64 (one sweep):
+// Causal forward.  One CTA takes 128 queries of one head and sweeps the keys in tiles of 64 (one sweep):
 //   S   = Q K_j^T       tcgen05.mma  M = 128, N = 64, K = d    -> 64 FP32 columns of tensor memory
 //   P_j = 2^(c S - m)   four warps, one query row per thread (its tensor-memory lane): no shuffles; the row
 //                       goes back to tensor memory as BF16 pairs, 32 columns (tcgen05.st)
@@ -677,7 +679,10 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 
 // ---- forward over key ranges ----------------------------------------------------------------------------------------
 // The products and buffers are the causal kernel's with heads of 128 (P_j over S_j), for both head sizes; one thread a query.
-// What bounds it are the row threads' multiply-adds (a capped score takes eight) and 2^x, which run on different units but come one
+// No unit is full.  By counters, of the cycles that an SM is at work (heads of 64, documents of 700, capped; heads of 128, 8192 tokens, biased):
+// instruction issue 43 / 44 %, FMA 37 / 23, 2^x 31 / 50, tensor pipe 15 / 50, with ten warps an SM: each of a scheduler's two or three
+// row warps takes its scores' multiply-adds (a capped score takes eight), 2^x, packing and stores one after the other, and a product of 64 keys
+// reads both operands from shared memory, 6 KB per 16 contraction steps, for half as long again as its tensor work.  So FMAs and 2^x come one
 // after the other where a tile's maximum has to be known before its first 2^x.  So a tile is taken relative to the query's reference
 // as it stands, scores and 2^x in one sweep, the maximum along with them; only where it turns out to lie above the reference by more
 // than 2^SCORED_SLACK (or where there is none yet) the tile is read again and taken in two sweeps, with a new reference.  The keys'
@@ -686,9 +691,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 // An infinity or NaN in V reaches all of a tile's queries in the product, those that do not see it by a probability of 0.  So a CTA
 // that finds something in its output that is no finite number goes over its tiles once more, and this time rids V of such values where
 // a tile has keys to mask, noting which keys they belong to.
-// 4 x 2048 tokens, us (TFLOP/s of what is visible): 32 / 8 heads of 64, causal 133 (519; the causal kernel 133), biased 143 (480), capped
-// 194 (354), documents of 700 tokens capped 157 (292); 16 / 8 heads of 128 85 (808), 91 (755), 114 (604).  1 x 8192, 16 heads of 128, biased, a
-// prefix: 264-284 (967-1042).
+// 4 x 2048 tokens, us (TFLOP/s of what is visible): 32 / 8 heads of 64, causal 132 (521; the causal kernel 133), biased 143 (481), capped
+// 195 (353); 16 / 8 heads of 128 87 (790), 91 (755), 115 (598).  1 x 8192, 16 heads of 128, biased, one document: 262-268 (1026-1049);
+// behind prefixes of up to 0.4 of the sequence, which it sees whole, 301-335.
 template <int HD> struct FwdScored {
   static constexpr int NP = HD / 64, Q_BYTES = NP * Q_PANEL, KV_BYTES = NP * KV_PANEL;
   static constexpr int OFF_K = Q_BYTES, OFF_V = OFF_K + 2 * KV_BYTES, OFF_CTL = OFF_V + 2 * KV_BYTES;
@@ -1025,7 +1030,9 @@ attn_fwd_scored_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
 // of P K (P times the cap's slope), a fourth product.  R's operand is written over dP, dS over S, as with heads of 128.  It costs the
 // fourth product and its operand's stores, dK / dV next to dQ, and with heads of 64 the overlap of a tile's score products with the
 // rows of the one before: forward and backward, 4 x 2048 tokens, 32 / 8 heads of 64, documents of 700, capped, 470 -> 501 us; 333 tokens, 4 / 2 heads
-// of 128, 24 -> 32.  Backward call, causal ranges, 414 us (the causal kernels 340), heads of 128 358 (341).
+// of 128, 24 -> 32.  Backward call, causal ranges, 408 us (the causal kernels 341), heads of 128 358 (332).  By counters, heads of 64, documents
+// of 700, capped: dQ / dK, dV issue 51 / 46 % of their cycles, FMA 47 / 34, tensor pipe 24 / 18; the long scoreboard, loads of
+// tensor memory among it, holds warps up longest.
 template <int HD> struct Dq {
   static constexpr int NP = HD / 64, Q_BYTES = NP * Q_PANEL, KV_BYTES = NP * KV_PANEL, STAGE = 2 * KV_BYTES, STAGES = 3;
   static constexpr int OFF_DO = Q_BYTES, OFF_KV = 2 * Q_BYTES, OFF_CTL = OFF_KV + STAGES * STAGE;
@@ -1170,7 +1177,9 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = *tmem_slot;                         // head_dim 64: S in columns 0..63, dP: 64..127, dQ: 128..191, dS (BF16 pairs): 192..223
+  // head_dim 64: S in columns 0..63, dP: 64..127, dQ: 128..191; causal: dS (BF16 pairs) in 192..223; over ranges: dS over S, R's operand
+  // over dP, R in 192..255.  head_dim 128: two S in 0..127, two dP in 128..255, dQ 256..383, over ranges R in 384..511; dS over S
+  const uint32_t tmem = *tmem_slot;
   if (FORM != CAUSAL || p.apart) faar_pdl_sync();
   else faar_pdl_launch();                                   // needs nothing of the dK / dV kernel, next to which it runs
   int2 range = {0, INT_MAX};                                // this thread's query
@@ -2045,9 +2054,11 @@ int launch_bwd(faar_ctx* ctx, TcBwdParams& p, const void* q, int64_t ldq, const 
   if (e) return e;
   const int tiles = (p.S + QT - 1) / QT;
   // Ranges make key tiles of any work, the longest of which the others wait for: with capped scores, whose items are long against what
-  // the exchange costs, heads of 64 deal up to twice as many.  4 x 2048 tokens, 32 / 8 heads of 64, us, one CTA a key tile -> two: documents of
-  // 700 tokens, capped 578 -> 485, one document each 591 -> 595, biased too 642 -> 649; before dQ came first, not capped 210 (documents of 200) ->
-  // 199, 396 -> 475; heads of 128 279 -> 318.
+  // the exchange costs, heads of 64 deal up to twice as many.  Backward call, one CTA a key tile -> two (where not said otherwise 4 x 2048
+  // tokens, 32 / 8 heads of 64), us: capped, documents of 700 tokens 534 -> 507, of 200 315 -> 286, one each 591 -> 587; 1 x 8192, documents of
+  // 700 634 -> 544, of 3000 1153 -> 920; 8 x 1000, of 300 323 -> 295; 3 x 2048, 8 / 8 heads, of 700 150 -> 136; biased too, of 700 587 ->
+  // 555, one each 642 -> 648.  Not capped, where it is left at one: of 700 377 -> 364, of 200 228 -> 210, one each 408 -> 420.  Heads of 128:
+  // capped, of 700 334 -> 376, one each 386 -> 424, not capped, of 200 171 -> 204.
   const int more = HD == 64 && (FORM & CAPPED) && (p.sc.key_lo || p.sc.key_hi) ? 2 : 1;
   p.parts = pick_parts(more * ctx->num_sms * Dkv<HD>::CTAS * Dkv<HD>::CTAS, tiles * p.Hkv * p.B, p.H / p.Hkv * ((p.S + KT - 1) / KT));
   auto launch_dq = [&] {

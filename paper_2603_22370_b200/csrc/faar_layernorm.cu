@@ -398,7 +398,10 @@ layernorm_dw_sum_kernel(const float* partials, int slabs, float* dg, float* db, 
 // thread make more groups, whose turns (a sum's latency, then another's work) overlap; a short row has no use for them.  Behind a sum
 // or not, the same shape: the same bits.  us, one vector -> two (-> four): forward 8192 x 2048 20.6 -> 18.2, 8192 x 4096 37.5 -> 31.8 (33.2), 16384 x
 // 1024 20.8 -> 18.1, with the sum 8192 x 4096 45.8 -> 49.6; backward 8192 x 2048 29.4 -> 27.3 (37.3), 8192 x 4096 49.0 -> 46.1 (61.4).
-// A plain copy of as many bytes as 8192 x 4096 forward takes 28.3.
+// A plain copy of as many bytes as 8192 x 4096 forward takes 24.9-28.3.  With a residual (forward) or its gradient (backward), 8192 x 2048
+// 24.0 and 32.8, 8192 x 4096 49.9 and 58.6, 777 x 1040 4.5 and 7.5.  By counters (8192 x 4096 forward, backward): instruction issue 63 and 67 %
+// of the cycles at work, ALU 33 and 44, FMA 31 and 37, DRAM 30 and 46: none is full, with 16 warps an SM that wait for their group's sums,
+// twice a row forward and once backward.
 struct Shape { int vpt, tpr, groups, ctas; };
 static_assert(4 * 8 * MAX_THREADS == FAAR_LAYERNORM_COLS, "four vectors a thread at the most");
 Shape shape(const faar_ctx* ctx, int rows, int cols) {
