@@ -385,8 +385,8 @@ __device__ __forceinline__ float2 add_bias(float2 x, float nb, float d) {
 
 // Rows of an operand that some of the rows working with it may not see: what is not finite there would reach them all, as 0 times
 // an infinity is no 0.  Such values of a staged tile are set to 0 (`units` 16-byte units from `base` on, of which the calling thread
-// takes every `threads`-th from `first` on; `found`: a flag in shared memory, set where there are any, or 0); the generic writes are made
-// visible to the tensor cores.
+// takes every `threads`-th from `first` on; `found`: a word in shared memory that gets `bits` where there are any, or 0); the generic
+// writes are made visible to the tensor cores.
 __device__ __forceinline__ bool not_finite(uint4 v) {        // all exponent bits of one of eight BF16 values set
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t acc = 0;
@@ -404,21 +404,23 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __noinline__ void scrub(uint32_t base, int units, int first, int threads, uint32_t found) {
+__device__ __noinline__ void scrub(uint32_t base, int units, int first, int threads, uint32_t found, uint32_t bits) {
   for (int u = first; u < units; u += threads) {
     const uint32_t at = base + 16u * (uint32_t)u;
     const uint4 v = lds128(at);
     if (!not_finite(v)) continue;
-    if (found) asm volatile("st.shared.u32 [%0], 1;" ::"r"(found) : "memory");
+    if (found) asm volatile("red.shared.or.b32 [%0], %1;" ::"r"(found), "r"(bits) : "memory");
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(only_finite(v.x)), "r"(only_finite(v.y)), "r"(only_finite(v.z)),
                  "r"(only_finite(v.w)) : "memory");
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
-__device__ __forceinline__ bool flagged(uint32_t flag) {
+// Tiles of KT rows where something was found: a bit each, modulo 32
+__device__ __forceinline__ uint32_t tile_bit(int tile) { return 1u << (tile & 31); }
+__device__ __forceinline__ uint32_t found_tiles(uint32_t found) {
   uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(flag) : "memory");
-  return v != 0;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(found) : "memory");
+  return v;
 }
 // Whether a row of HD values in memory holds one that is not finite
 template <int HD>
@@ -860,7 +862,7 @@ attn_fwd_scored_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
           const uint32_t low = reinterpret_cast<volatile uint32_t*>(seen)[0], high = reinterpret_cast<volatile uint32_t*>(seen)[1];
           if (low | high) {
             poison |= ((low & range_bits(range, k0)) | (high & range_bits(range, k0 + 32))) != 0u;
-            scrub(sV(st), KV_BYTES / 16, threadIdx.x, 128, 0u);
+            scrub(sV(st), KV_BYTES / 16, threadIdx.x, 128, 0u, 0u);
           }
         }
         // S_j complete, and with it all products issued before, P V_{j-2} among them: of the two barriers for P V the one of tile j - 1
@@ -1107,15 +1109,25 @@ __device__ __forceinline__ void turn_back(const float2* angles, long long tokens
   }
 }
 
+// Barriers of the row threads; the second says whether one of them has x
+__device__ __forceinline__ void row_threads_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(ROW_THREADS) : "memory"); }
+__device__ __forceinline__ bool row_threads_any(bool x) {
+  uint32_t any;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(any) : "r"((uint32_t)x), "n"(ROW_THREADS) : "memory");
+  return any != 0;
+}
+
 // What was taken out of a staged row of K for those who do not see it, those who do get all the same: a row of dS K with such a key is no
 // number, whatever dS is (0 times an infinity, too).  Tiles that all of a CTA's queries see get there by themselves; where an edge tile's
-// were set to 0, this looks at the keys of the CTA's span once more, in memory: whether one that the thread's query (`range`) sees has one.
-// All row threads call it; `words`: 8 ints of shared memory.
-__device__ __forceinline__ void row_threads_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(ROW_THREADS) : "memory"); }
+// were set to 0 (`found`), this looks at the keys of the CTA's span in those tiles once more, in memory: whether one that the thread's query
+// (`range`) sees has one.  All row threads call it; `words`: 8 ints of shared memory.
 template <int HD>
-__device__ __noinline__ bool sees_bad_key(const __nv_bfloat16* k, long long ldk, Span span, int2 range, volatile uint32_t* words) {
+__device__ __noinline__ bool sees_bad_key(const __nv_bfloat16* k, long long ldk, Span span, int2 range, uint32_t found,
+                                          volatile uint32_t* words) {
   bool sees = false;
-  for (int k0 = span.lo; k0 < span.hi; k0 += ROW_THREADS) {
+  for (int k0 = span.lo / KT * KT; k0 < span.hi; k0 += ROW_THREADS) {
+    if (!(__funnelshift_r(found, found, k0 / KT) & ((1u << (ROW_THREADS / KT)) - 1u))) continue;
     const int key = k0 + (int)threadIdx.x;
     const uint32_t bad = __ballot_sync(0xffffffffu, key < span.hi && row_not_finite<HD>(k + key * ldk));
     row_threads_sync();                                     // the words of the keys before have been read
@@ -1146,7 +1158,7 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   auto kvfull = [&](int s) { return ctl + 8u + 8u * s; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_CTL + 96);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 100);
-  const uint32_t scrubbed = ctl + 224;                       // over ranges: K had something that is not finite
+  const uint32_t scrubbed = ctl + 224;                       // over ranges: tiles of K that had something not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // one-dimensional grid, query tile slowest and descending: CTAs start in order of decreasing work
@@ -1341,7 +1353,8 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const int st = j % C::STAGES;
             ok = bar_wait(kvfull(st), (uint32_t)((j / C::STAGES) & 1), abort_flag, 0xD15u);
 #pragma unroll
-            for (int c = 0; c < C::NP; ++c) scrub(sK(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, 32 * (warp & 3) + lane, 128, scrubbed);
+            for (int c = 0; c < C::NP; ++c) scrub(sK(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, 32 * (warp & 3) + lane, 128, scrubbed,
+                                                tile_bit(kt0 + j));
           }
         }
         if constexpr ((FORM & CAPPED) != 0) tanh_values(t, p.sc);
@@ -1419,7 +1432,8 @@ attn_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       __syncthreads();
       if (ok) by = half == 0 ? mine + sums[QT + row] : sums[row] + mine;
       if (ok && half == 0 && qi < p.S) const_cast<float*>(p.dsum)[ro + qi] = (by - nd) / p.inv_sqrt_d;
-      if (flagged(scrubbed) && sees_bad_key<HD>(p.k + seq0 * p.ldk + g * HD, p.ldk, span, range, reinterpret_cast<volatile uint32_t*>(sums + 2 * QT)))
+      const uint32_t found = found_tiles(scrubbed);
+      if (found && sees_bad_key<HD>(p.k + seq0 * p.ldk + g * HD, p.ldk, span, range, found, reinterpret_cast<volatile uint32_t*>(sums + 2 * QT)))
         by = __int_as_float(0x7FFFFFFF);
     }
     if (ok) {
@@ -1577,9 +1591,11 @@ __device__ __forceinline__ void spoil(uint32_t t, bool bad) {
   wait_st();
 }
 // As sees_bad_key: what was taken out of staged rows of Q or dO for the keys that they do not see makes dK or dV of those that they do
-// no number.  Goes through the queries of all heads of the group once more, in memory, and spoils the accumulators of this CTA's keys
-// that one with such a row sees.  All row threads call it, the products being through.  It finds anew what it works on: with arguments
-// whole and dealt key tiles of heads of 64 kept their registers for them (4 x 2048 tokens, capped, backward call 597 -> 615 us).
+// no number.  Goes through the queries that see a key of this CTA's, in the tiles where that was, once more, in memory, and spoils the
+// accumulators of the keys that one with such a row sees.  All row threads call it, the products being through.  It finds anew what it
+// works on: with arguments whole and dealt key tiles of heads of 64 kept their registers for them (4 x 2048 tokens, capped, backward call
+// 597 -> 615 us).  Sequences that end in 100 tokens of padding, finite -> NaN, backward call, us: 4 x 2048 tokens, heads of 64 409 -> 442, of 128
+// 350 -> 394, 1 x 8192 capped 1965 -> 2154 (all tiles looked through: 1283, 1212, 8721).
 template <int HD, bool DEALT>
 __device__ __noinline__ void spoil_seen(const TcBwdParams& p) {
   extern __shared__ uint8_t raw[];
@@ -1588,26 +1604,28 @@ __device__ __noinline__ void spoil_seen(const TcBwdParams& p) {
   const uint32_t t_lane = *reinterpret_cast<volatile uint32_t*>(smem + Dkv<HD>::OFF_CTL + 128) + ((threadIdx.x & 96) << 16);
   const int groups = p.Hkv * p.B, rep = p.H / p.Hkv, tile = (int)(blockIdx.x / (unsigned)(DEALT ? p.parts : 1));
   const int g = (tile % groups) % p.Hkv, b = (tile % groups) / p.Hkv, row = (int)threadIdx.x & (QT - 1), half = (int)threadIdx.x >> 7;
-  const int kj = tile / groups * QT + row;
+  const int k0 = tile / groups * QT, kj = k0 + row;
+  const uint32_t found = found_tiles(s32(smem) + Dkv<HD>::OFF_CTL + 136);
   int seen = 0;                                             // by a query whose q (1), whose dO (2) is not finite
-  for (int h = g * rep; h < (g + 1) * rep; ++h)
-    for (int q0 = 0; q0 < p.S; q0 += ROW_THREADS) {
-      const int q = q0 + (int)threadIdx.x;
-      int4 mine = make_int4(EMPTY_LO, 0, 0, 0);             // first key, how many, which of the two is not finite
-      if (q < p.S) {
-        const int2 r = key_range(p.sc, b, q, p.S);
-        const long long at = (long long)b * p.S + q;
-        mine = make_int4(r.x, max(r.y - r.x, 0), row_not_finite<HD>(p.q + at * p.ldq + h * HD) + 2 * row_not_finite<HD>(p.dout + at * p.ldo + h * HD), 0);
-      }
-      row_threads_sync();                                   // the list before has been read
+  for (int q0 = 0; q0 < p.S; q0 += ROW_THREADS) {
+    if (!(__funnelshift_r(found, found, q0 / KT) & ((1u << (ROW_THREADS / KT)) - 1u))) continue;
+    const int q = q0 + (int)threadIdx.x;
+    const int2 r = q < p.S ? key_range(p.sc, b, q, p.S) : make_int2(EMPTY_LO, EMPTY_HI);
+    const bool near = r.x < k0 + QT && r.y > k0;            // sees a key of the tile
+    const long long at = (long long)b * p.S + q;
+    for (int h = g * rep; h < (g + 1) * rep; ++h) {
+      int4 mine = make_int4(r.x, r.y - r.x, 0, 0);          // first key, how many, which of the two is not finite
+      if (near) mine.z = row_not_finite<HD>(p.q + at * p.ldq + h * HD) + 2 * row_not_finite<HD>(p.dout + at * p.ldo + h * HD);
+      if (!row_threads_any(mine.z != 0)) continue;          // (the list before has been read)
       list[threadIdx.x] = mine;
       row_threads_sync();
 #pragma unroll 1
       for (int i = 0; i < ROW_THREADS; ++i) {
         const int4 v = list[i];
-        if ((uint32_t)(kj - v.x) < (uint32_t)v.y) seen |= v.z;
+        if (v.z && (uint32_t)(kj - v.x) < (uint32_t)v.y) seen |= v.z;
       }
     }
+  }
   fence_after();
   const uint32_t t_half = t_lane + (uint32_t)(HD / 2 * half);
   if (__any_sync(0xffffffffu, seen & 1)) spoil<HD>(t_half + (uint32_t)Dkv<HD>::COL_DK, seen & 1);
@@ -1634,7 +1652,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   auto bar_rv = [&](int s) { return ctl + 112u + 8u * s; };       // 2: lse / delta of an item staged, previous use read by all
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_CTL + 128);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_CTL + 132);
-  const uint32_t scrubbed = ctl + 136;                   // over ranges: Q or dO had something that is not finite
+  const uint32_t scrubbed = ctl + 136;                   // over ranges: tiles of Q or dO that had something not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // one-dimensional grid, key tile slowest: CTAs start in order of decreasing work (the first key tiles see the
@@ -1875,8 +1893,8 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             ok = bar_wait(qfull(st), (uint32_t)((i / C::STAGES) & 1), abort_flag, 0xF15u);
 #pragma unroll
             for (int c = 0; c < C::NP; ++c) {
-              scrub(sQ(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed);
-              scrub(sDO(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed);
+              scrub(sQ(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed, tile_bit(q0 / KT));
+              scrub(sDO(st) + (uint32_t)(c * KV_PANEL + 4096 * half), 256, row, 128, scrubbed, tile_bit(q0 / KT));
             }
           }
         }
@@ -1935,7 +1953,7 @@ attn_dkv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     if constexpr (FORM != CAUSAL) {
       row_threads_sync();                                     // all have come to the end: the flag is final, the operands have been read
-      if (flagged(scrubbed)) spoil_seen<HD, DEALT>(p);
+      if (found_tiles(scrubbed)) spoil_seen<HD, DEALT>(p);
     }
     if constexpr (DEALT) {
       fence_after();

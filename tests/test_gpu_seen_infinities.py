@@ -120,3 +120,20 @@ def test_an_infinite_query_leaves_no_gradient_to_the_keys_that_it_sees(ctx, D, c
             assert torch.equal(got[i][rest][:, cols], clean[i][rest][:, cols])
     if cap:
         assert torch.isfinite(got[4]).all() and torch.isfinite(got[2]).all() and torch.isfinite(got[0]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("which", ["k", "q", "do"])
+@pytest.mark.parametrize("at", [2111, 2240, 4299])
+def test_tiles_far_into_a_sequence(ctx, D, which, at):  # noqa: F811
+    """The same beyond 32 tiles, with edge tiles in the middle and the diagonal's."""
+    n, cut = 4300, 2139
+    c = Case(1, n, 4, 2, D, *ranges_of_two_documents(n, cut), 20.0, pad=0)
+    clean, got = runs(ctx, c, which, at, INF)
+    first, last = (0, cut) if at < cut else (cut, n)
+    heads, own = {"k": (4, 2), "q": (2, 3), "do": (2, 4)}[which]
+    hit = list(range(at, last) if which == "k" else range(first, at + 1))
+    rest = sorted(set(range(n)) - set(hit))
+    for h in range(heads):
+        cols = slice(h * D, (h + 1) * D)
+        assert broken(got[own][hit][:, cols]).all() and torch.equal(got[own][rest][:, cols], clean[own][rest][:, cols])
